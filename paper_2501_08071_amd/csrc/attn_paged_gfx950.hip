@@ -185,14 +185,14 @@ template <int D, int KB, int N> struct Pager {
                 const int j = ROWS * (first + i), e = from + (np_shift ? j >> c.page_shift : 0);
                 const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)at, e);
                 const uint32_t hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)((uint64_t)at >> 32), e);
-                lds_dma16(lds + 1024 * i, base + ((uint64_t)hi << 32 | lo) + ((kb * KB + j) & mask) * ROW, part[i % KINDS]);
+                lds_dma16(lds + 1024 * i, base + ((uint64_t)hi << 32 | lo) + paged_key_offset(kb * KB + j, mask, ROW), part[i % KINDS]);
             }
         } else {
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 const int j = ROWS * (first + i) + 16 * lane / ROW;
                 const long long page = __shfl(at, from + (j >> c.page_shift), 64);
-                dma16(lds + 1024 * i, base + page + ((kb * KB + j) & mask) * ROW + (part[i % KINDS] & (ROW - 1)));
+                dma16(lds + 1024 * i, base + page + paged_key_offset(kb * KB + j, mask, ROW) + (part[i % KINDS] & (ROW - 1)));
             }
         }
     }

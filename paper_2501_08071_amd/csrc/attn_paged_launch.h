@@ -14,6 +14,10 @@ struct PagedCache {
     int n_pages, page_shift, Hk, table_stride, width, B, T;
 };
 
+// Bytes from the first key of a head in a page to key j of a sequence, of row_bytes each; mask: the page's keys - 1.  In 64 bits: a page of
+// 2^24 keys of 256 bytes is 4 GiB.
+__host__ __device__ inline uint64_t paged_key_offset(int j, int mask, int row_bytes) { return (uint64_t)(uint32_t)(j & mask) * (uint32_t)row_bytes; }
+
 struct AppendLaunch {
     PagedCache c;
     const void *q, *k, *v;    // tokens q_stride, k_stride, v_stride elements apart

@@ -8,3 +8,4 @@ extern "C" void plan(int B, int T, int Hq, int Hk, int D, int max_q, int max_kv,
     const long long v[] = {p.rows, p.workgroups, p.balanced, p.direct, p.waves, p.prefix_rows, p.prefix_tiles, p.prefix_splits, p.bytes, p.part_floats, p.prefix_floats};
     for (int i = 0; i < 11; ++i) out[i] = v[i];
 }
+extern "C" long long key_offset(int j, int mask, int row_bytes) { return (long long)paged_key_offset(j, mask, row_bytes); }

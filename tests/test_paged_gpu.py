@@ -263,6 +263,43 @@ def test_a_cache_past_32_bits_and_a_long_sequence():
             assert ((lse[t, 4 * h:4 * h + 4].double() - torch.logsumexp(x, 1)).abs() <= 1e-3).all()
 
 
+@pytest.mark.parametrize("D,Hq", [(128, 4), (64, 2)])
+def test_a_page_past_32_bits(D, Hq):
+    """A page of more than 2^31 bytes: what is stored past its first 2^31 is what is read back, by one token, by some, as a prefix.  The keys in
+    front are zeros, with logit 0 and value 0; those at the end have logits around 30, and outweigh them."""
+    front, n, dtype = 2 ** 32 // (2 * D), 40, BF16             # keys of 2^32 bytes
+    page = 2 * front
+    g = torch.Generator(device="cuda").manual_seed(D)
+    kc, vc = (torch.zeros(1, 1, page, D, dtype=dtype, device="cuda") for _ in range(2))
+    scale = D ** -0.5
+    q = (1.0 + 0.3 * torch.randn(n, Hq, D, device="cuda", generator=g)).to(dtype)
+    k = (30.0 / (scale * D) + 0.3 * torch.randn(n, 1, D, device="cuda", generator=g)).to(dtype)
+    v = torch.randn(n, 1, D, device="cuda", generator=g).to(dtype)
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    table = torch.zeros(1, 1, dtype=torch.int32, device="cuda")
+    P.attn_kv_append(None, k, v, kc, vc, table, i32(0, n), i32(front + n))
+    assert torch.equal(kc[0, 0, front:front + n], k[:, 0]) and torch.equal(vc[0, 0, front:front + n], v[:, 0])
+
+    def expected(rows, sees):
+        """Rows of q, the first of the keys at the end that each sees."""
+        z = scale * q[rows].double() @ k[:, 0].double().T
+        hidden = torch.arange(n, device="cuda")[None, None, :] >= torch.tensor(sees, device="cuda")[:, None, None]
+        w = z.masked_fill(hidden, -math.inf).exp()
+        total = w.sum(-1) + front
+        vd = v[:, 0].double()
+        size = scale * (q[rows].double().abs() @ k[:, 0].double().abs().T).amax(-1)
+        return [t.cpu() for t in (w @ vd / total[..., None], total.log(), w @ vd.abs() / total[..., None], torch.zeros(len(rows), Hq, D), size)]
+
+    last = list(range(n - 1, n))
+    got = P.attn_paged_fwd(q[last], kc, vc, table, i32(0, 1), i32(front + n), scale, max_q=1)
+    check(got, expected(last, [n]), dtype)
+    got = P.attn_paged_fwd(q, kc, vc, table, i32(0, n), i32(front + n), scale, max_q=n)
+    check(got, expected(list(range(n)), [i + 1 for i in range(n)]), dtype)
+    for rows in (last, list(range(n))):
+        got = P.attn_paged_fwd(q[rows], kc, vc, table, i32(0, len(rows)), i32(0), scale, max_q=len(rows), prefix_table=table[0], prefix_len=front + n)
+        check(got, expected(rows, [n] * len(rows)), dtype)
+
+
 def test_what_non_finite_values_do():
     """A NaN key, an infinite value: in the rows that see them and no others of other sequences; rows that repeat bit for bit."""
     s = make([1, 1, 1], [100, 100, 100], 2, 1, 64, 16, BF16, seed=9)

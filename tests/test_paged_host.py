@@ -125,3 +125,13 @@ def test_the_norm_refuses():
     for name in "x r w y s ro".split():
         assert call(**{name: OK + 8}) == -6
     assert call(n=0, x=0, r=0, w=0, y=0, s=0, ro=0) == 0
+
+
+@pytest.mark.parametrize("D", [32, 64, 128])
+def test_a_key_s_place_in_a_page_of_any_size(L, D):
+    """Pages of up to 2^30 keys are accepted: a key's place in one passes 32 bits."""
+    L.key_offset.restype = ctypes.c_longlong
+    for shift in range(31):
+        size = 1 << shift
+        for j in {0, 1, size // 2, size - 1, size, (1 << 23) - 1, 1 << 23, (1 << 23) + 77, 1 << 24, (1 << 30) - 1}:
+            assert L.key_offset(j, size - 1, 2 * D) == j % size * 2 * D, (shift, j)
