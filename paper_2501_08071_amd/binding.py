@@ -121,6 +121,20 @@ def _load_fast():
 _fast = _load_fast()
 
 
+def _new(shape, dtype, device, stream, returned=True):
+    """Memory that a call on `stream` (None: the current one) writes.  For another stream it comes from that stream's own pool: what is free in the current
+    one's may still be written by work under way there, for which `stream` does not wait.  A result (`returned`) is then told of the current
+    stream, where it is likely to be read: it is not handed out again before that is done."""
+    current = torch.cuda.current_stream(device)
+    if stream is None or stream == current:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    if returned:
+        t.record_stream(current)
+    return t
+
+
 def attn_status_str(status: int) -> str:
     return lib.attn_status_str(int(status)).decode()
 
@@ -294,9 +308,9 @@ def attn_fwd(q, k, v, causal: bool, scale: float, o=None, lse=None, stream=None,
     B, H, S, D = q.shape
     odt = q.dtype if _o16 else torch.float32
     if o is None:
-        o = torch.empty((B, H, S, D), dtype=odt, device=q.device)
+        o = _new((B, H, S, D), odt, q.device, stream)
     if lse is None and want_lse:
-        lse = torch.empty((B, H, S), dtype=torch.float32, device=q.device)
+        lse = _new((B, H, S), torch.float32, q.device, stream)
     for t, shp, dt in ((o, (B, H, S, D), odt), (lse, (B, H, S), torch.float32)):
         if t is not None and (t.dtype != dt or tuple(t.shape) != shp or not t.is_contiguous() or not t.is_cuda):
             raise ValueError("o / lse must be contiguous device tensors of shape [B,H,S,D] / [B,H,S] (lse fp32; o fp32, "
@@ -394,7 +408,7 @@ def attn_kv_append(q, k, v, k_cache, v_cache, page_table, cu_q, kv_len, cos=None
     if q is None:
         q_out = None
     elif q_out is None:
-        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        q_out = _new(q.shape, q.dtype, q.device, stream)
     elif q_out.shape != q.shape or not q_out.is_cuda or not q_out.is_contiguous():
         raise ValueError("q_out must be a contiguous device tensor of q's shape")
     rot = n_angles = 0
@@ -446,24 +460,21 @@ def attn_paged_fwd(q, k_cache, v_cache, page_table, cu_q, kv_len, scale: float, 
             raise ValueError("prefix_table must hold the pages of prefix_len keys")
         _ints(prefix_table, "prefix_table", (None,))
     if o is None:
-        o = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        o = _new(q.shape, q.dtype, q.device, stream)
     if lse is None and want_lse:
-        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
+        lse = _new(q.shape[:2], torch.float32, q.device, stream)
     for t, shp, dt in ((o, q.shape, q.dtype), (lse, q.shape[:2], torch.float32)):
         if t is not None and (t.dtype != dt or t.shape != shp or not t.is_contiguous() or not t.is_cuda):
             raise ValueError("o / lse must be contiguous device tensors [T, Hq, D] of q's dtype / [T, Hq] fp32")
-    current = torch.cuda.current_stream(q.device)
-    on = stream or current
     need = max(0, attn_paged_workspace(cache.B, T, Hq, cache.Hk, D, max_q, max_kv, prefix_len))
     if workspace is None:
-        workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
-        if on != current:      # its memory goes back to the current stream's pool: not before the other stream is done with it
-            workspace.record_stream(on)
+        workspace = _new(need, torch.uint8, q.device, stream, returned=False)
     elif workspace.dtype != torch.uint8 or not workspace.is_cuda or not workspace.is_contiguous():
         raise ValueError("workspace must be a contiguous uint8 device tensor")
+    st = (stream or torch.cuda.current_stream(q.device)).cuda_stream
     rc = attn_paged_fwd_raw(cache, q.data_ptr(), qs, o.data_ptr(), lse.data_ptr() if lse is not None else 0,
                             prefix_table.data_ptr() if prefix_len else 0, prefix_len, Hq, max_q, max_kv, scale, workspace.data_ptr(),
-                            workspace.numel(), on.cuda_stream)
+                            workspace.numel(), st)
     if rc != 0:
         raise AttnError(rc, attn_status_str(rc), "attn_paged_fwd")
     return o, lse
@@ -496,7 +507,7 @@ def rmsnorm_fwd_raw(x_ptr, w_ptr, y_ptr, n_rows, d, eps, dtype, stream) -> int:
                                stream or None))
 
 
-def _row_args(x, y):
+def _row_args(x, y, stream):
     if x.dtype == torch.float16:
         dtype = F16
     elif x.dtype == torch.bfloat16:
@@ -506,7 +517,7 @@ def _row_args(x, y):
     if x.dim() < 1 or not x.is_cuda or not x.is_contiguous():
         raise ValueError("x must be a contiguous device tensor with the rows along the last dimension")
     if y is None:
-        y = torch.empty_like(x)
+        y = _new(x.shape, x.dtype, x.device, stream)
     elif y.dtype != x.dtype or y.shape != x.shape or not y.is_cuda or not y.is_contiguous():
         raise ValueError("y must be a contiguous device tensor of the shape and dtype of x")
     n = x.shape[-1]
@@ -518,7 +529,7 @@ def softmax_rows_fwd(x, y=None, stream=None):
     done = _fast.softmax_rows_fwd(x, y, stream)
     if done is not None:
         return done
-    dtype, y, n_rows, n = _row_args(x, y)
+    dtype, y, n_rows, n = _row_args(x, y, stream)
     st = (stream or torch.cuda.current_stream(x.device)).cuda_stream
     rc = softmax_rows_fwd_raw(x.data_ptr(), y.data_ptr(), n_rows, n, dtype, st)
     if rc != 0:
@@ -531,7 +542,7 @@ def rmsnorm_fwd(x, w, eps: float, y=None, stream=None):
     done = _fast.rmsnorm_fwd(x, w, eps, y, stream)
     if done is not None:
         return done
-    dtype, y, n_rows, n = _row_args(x, y)
+    dtype, y, n_rows, n = _row_args(x, y, stream)
     if w.dtype != x.dtype or tuple(w.shape) != (n,) or not w.is_cuda or not w.is_contiguous():
         raise ValueError("w must be a contiguous device tensor [d] of x's dtype")
     st = (stream or torch.cuda.current_stream(x.device)).cuda_stream
@@ -548,24 +559,26 @@ def residual_rmsnorm_fwd_raw(x_ptr, r_ptr, w_ptr, y_ptr, scale_ptr, r_out_ptr, n
 
 
 def _residual_norm(x, r, w, eps, fp8, group, y, scale, r_out, stream):
-    dtype, _, n_rows, n = _row_args(x, None if fp8 else y)
+    dtype, y16, n_rows, n = _row_args(x, x if fp8 else y, stream)
     if w.dtype != x.dtype or tuple(w.shape) != (n,) or not w.is_cuda or not w.is_contiguous():
         raise ValueError("w must be a contiguous device tensor [d] of x's dtype")
     if r is None:
         r_out = None
     elif r_out is None:
-        r_out = torch.empty_like(x)
+        r_out = _new(x.shape, x.dtype, x.device, stream)
     for t in (r, r_out):
         if t is not None and (t.dtype != x.dtype or t.shape != x.shape or not t.is_cuda or not t.is_contiguous()):
             raise ValueError("r and r_out must be contiguous device tensors of the shape and dtype of x")
-    if y is None:
-        y = torch.empty(x.shape, dtype=torch.float8_e4m3fn if fp8 else x.dtype, device=x.device)
+    if not fp8:
+        y = y16
+    elif y is None:
+        y = _new(x.shape, torch.float8_e4m3fn, x.device, stream)
     if fp8:
         if y.dtype != torch.float8_e4m3fn or y.shape != x.shape or not y.is_cuda or not y.is_contiguous():
             raise ValueError("y must be a contiguous float8_e4m3fn device tensor of the shape of x")
         shape = (*x.shape[:-1], -(-n // int(group)) if group else 1)
         if scale is None:
-            scale = torch.empty(shape, dtype=torch.float32, device=x.device)
+            scale = _new(shape, torch.float32, x.device, stream)
         elif scale.dtype != torch.float32 or scale.shape != shape or not scale.is_cuda or not scale.is_contiguous():
             raise ValueError("scale must be a contiguous float32 device tensor [..., 1], or [..., ceil(d / group)]")
     st = (stream or torch.cuda.current_stream(x.device)).cuda_stream
@@ -646,7 +659,7 @@ def gemm_leakyrelu_fwd(a, b, slope: float = 0.01, c=None, stream=None):
     N = b3.shape[2]
     shape = (batch, M, N) if a.dim() == 3 else (M, N)
     if c is None:
-        c = torch.empty(shape, dtype=a.dtype, device=a.device)
+        c = _new(shape, a.dtype, a.device, stream)
     elif c.dtype != a.dtype or tuple(c.shape) != shape or not c.is_cuda or not c.is_contiguous():
         raise ValueError("c must be a contiguous device tensor [batch, M, N] of the dtype of a")
     st = (stream or torch.cuda.current_stream(a.device)).cuda_stream

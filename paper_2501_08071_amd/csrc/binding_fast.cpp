@@ -12,6 +12,8 @@
 #include <ATen/core/Tensor.h>
 #include <ATen/ops/empty.h>
 #include <ATen/PythonTorchFunctionTLS.h>
+#include <c10/hip/HIPCachingAllocator.h>
+#include <c10/hip/HIPGuard.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -59,17 +61,25 @@ bool flag(PyObject* o, int& x) {
     x = PyObject_IsTrue(o);
     return true;
 }
-// the stream handle: of the torch stream given, or of the current one on t's device
-bool stream_of(PyObject* o, const at::Tensor& t, void*& st) {
-    if (o == Py_None) {
-        st = c10::hip::getCurrentHIPStream(t.device().index()).stream();
-        return true;
-    }
+// Where a call goes: the torch stream given, or the current one on t's device.
+struct Where {
+    void* handle;
+    bool elsewhere;             // not the current stream
+    c10::DeviceIndex device;
+};
+bool stream_of(PyObject* o, const at::Tensor& t, Where& w) {
+    w.device = t.device().index();
+    w.handle = c10::hip::getCurrentHIPStream(w.device).stream();
+    w.elsewhere = false;
+    if (o == Py_None) return true;
     PyObject* h = PyObject_GetAttrString(o, "cuda_stream");
     if (h == nullptr) return false;
-    st = PyLong_AsVoidPtr(h);
+    void* given = PyLong_AsVoidPtr(h);
     Py_DECREF(h);
-    return !PyErr_Occurred();
+    if (PyErr_Occurred()) return false;
+    w.elsewhere = given != w.handle;
+    w.handle = given;
+    return true;
 }
 
 // Launching and allocating may wait for the GPU, and what the GPU waits for may be Python's (a host function in a stream):
@@ -78,9 +88,20 @@ struct NoLock {
     PyThreadState* s = PyEval_SaveThread();
     ~NoLock() { PyEval_RestoreThread(s); }
 };
-at::Tensor new_tensor(at::IntArrayRef sizes, const at::TensorOptions& opt) {
+// Memory that a call on w writes, for another stream than the current one from that stream's own pool: what is free in the current one's may
+// still be written by work under way there, for which the other does not wait.  A result (`returned`) is then told of the current stream, where it
+// is likely to be read: it is not handed out again before that is done.
+at::Tensor new_tensor(at::IntArrayRef sizes, const at::TensorOptions& opt, const Where& w, bool returned = true) {
     NoLock _;
-    return at::empty(sizes, opt.requires_grad(false));
+    if (!w.elsewhere) return at::empty(sizes, opt.requires_grad(false));
+    const auto current = c10::hip::getCurrentHIPStream(w.device);
+    at::Tensor t;
+    {
+        c10::hip::HIPStreamGuard there(c10::hip::getStreamFromExternal((hipStream_t)w.handle, w.device));
+        t = at::empty(sizes, opt.requires_grad(false));
+    }
+    if (returned) c10::hip::HIPCachingAllocator::recordStream(t.storage().data_ptr(), current);
+    return t;
 }
 
 // What any of the functions below may throw (memory for an output, a device that is gone) is left to binding.py's own way.
@@ -120,17 +141,17 @@ PyObject* fast_attn(PyObject*, PyObject* const* a, Py_ssize_t n) {
         if (!fits_int(z[0]) || !fits_int(z[1]) || !fits_int(z[2]) || !fits_int(z[3])) return nullptr;
         int causal, want_lse, o16, rc;
         double scale;
-        void* st;
-        if (!flag(a[3], causal) || !real(a[4], scale) || !flag(a[8], want_lse) || !flag(a[9], o16) || !stream_of(a[7], *q, st)) return nullptr;
+        Where w;
+        if (!flag(a[3], causal) || !real(a[4], scale) || !flag(a[8], want_lse) || !flag(a[9], o16) || !stream_of(a[7], *q, w)) return nullptr;
         const auto odt = o16 ? q->scalar_type() : at::kFloat;
         at::Tensor o_new, lse_new;
         const at::Tensor *o, *lse = nullptr;
-        if (a[5] == Py_None) o = &(o_new = new_tensor(z, q->options().dtype(odt)));
+        if (a[5] == Py_None) o = &(o_new = new_tensor(z, q->options().dtype(odt), w));
         else if (!(o = gpu_tensor(a[5])) || o->scalar_type() != odt || o->sizes() != z) return nullptr;
         if (a[6] != Py_None) {
             if (!(lse = gpu_tensor(a[6])) || lse->scalar_type() != at::kFloat || lse->sizes() != z.slice(0, 3)) return nullptr;
         } else if (want_lse) {
-            lse = &(lse_new = new_tensor(z.slice(0, 3), q->options().dtype(at::kFloat)));
+            lse = &(lse_new = new_tensor(z.slice(0, 3), q->options().dtype(at::kFloat), w));
         }
         float* l = lse ? (float*)lse->mutable_data_ptr() : nullptr;
         const int B = (int)z[0], H = (int)z[1], S = (int)z[2], D = (int)z[3];
@@ -138,8 +159,8 @@ PyObject* fast_attn(PyObject*, PyObject* const* a, Py_ssize_t n) {
         void* op = o->mutable_data_ptr();
         {
             NoLock _;
-            rc = o16 ? abi.attn_o16(qp, kp, vp, op, l, B, H, S, D, causal, (float)scale, dt, st)
-                     : abi.attn(qp, kp, vp, (float*)op, l, B, H, S, D, causal, (float)scale, dt, st);
+            rc = o16 ? abi.attn_o16(qp, kp, vp, op, l, B, H, S, D, causal, (float)scale, dt, w.handle)
+                     : abi.attn(qp, kp, vp, (float*)op, l, B, H, S, D, causal, (float)scale, dt, w.handle);
         }
         if (rc != 0) return nullptr;
         PyObject* po = a[5] != Py_None ? Py_NewRef(a[5]) : THPVariable_Wrap(o_new);
@@ -151,13 +172,13 @@ PyObject* fast_attn(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
-// x [..., d] and y of its shape and type (allocated if None); the rows
-const at::Tensor* row_operands(PyObject* px, PyObject* py, at::Tensor& y_new, const at::Tensor*& y, long long& rows, int& d, int& dt) {
+// x [..., d] and y of its shape and type (allocated if None); the rows, and where to
+const at::Tensor* row_operands(PyObject* px, PyObject* py, PyObject* ps, at::Tensor& y_new, const at::Tensor*& y, long long& rows, int& d, int& dt, Where& w) {
     const at::Tensor* x = gpu_tensor(px);
-    if (!x || (dt = type_of(*x)) < 0 || x->dim() < 1) return nullptr;
+    if (!x || (dt = type_of(*x)) < 0 || x->dim() < 1 || !stream_of(ps, *x, w)) return nullptr;
     const int64_t n = x->sizes().back();
     if (!fits_int(n)) return nullptr;
-    if (py == Py_None) y = &(y_new = new_tensor(x->sizes(), x->options()));
+    if (py == Py_None) y = &(y_new = new_tensor(x->sizes(), x->options(), w));
     else if (!(y = gpu_tensor(py)) || y->scalar_type() != x->scalar_type() || y->sizes() != x->sizes()) return nullptr;
     d = (int)n;
     rows = n ? x->numel() / n : 0;
@@ -172,10 +193,10 @@ PyObject* fast_softmax(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const at::Tensor* y;
         long long rows;
         int d, dt;
-        void* st;
-        const at::Tensor* x = row_operands(a[0], a[1], y_new, y, rows, d, dt);
-        if (!x || !stream_of(a[2], *x, st)) return nullptr;
-        if (launched([&](void* xp, void* yp) { return abi.softmax(xp, yp, rows, d, dt, st); }, *x, *y)) return given_or_new(a[1], y_new);
+        Where s;
+        const at::Tensor* x = row_operands(a[0], a[1], a[2], y_new, y, rows, d, dt, s);
+        if (!x) return nullptr;
+        if (launched([&](void* xp, void* yp) { return abi.softmax(xp, yp, rows, d, dt, s.handle); }, *x, *y)) return given_or_new(a[1], y_new);
         return nullptr;
     });
 }
@@ -187,12 +208,12 @@ PyObject* fast_rmsnorm(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const at::Tensor* y;
         long long rows;
         int d, dt;
-        void* st;
+        Where s;
         double eps;
-        const at::Tensor *x = row_operands(a[0], a[3], y_new, y, rows, d, dt), *w = gpu_tensor(a[1]);
+        const at::Tensor *x = row_operands(a[0], a[3], a[4], y_new, y, rows, d, dt, s), *w = gpu_tensor(a[1]);
         if (!x || !w || w->scalar_type() != x->scalar_type() || w->dim() != 1 || w->sizes()[0] != d) return nullptr;
-        if (!real(a[2], eps) || !stream_of(a[4], *x, st)) return nullptr;
-        if (launched([&](void* xp, void* wp, void* yp) { return abi.rmsnorm(xp, wp, yp, rows, d, (float)eps, dt, st); }, *x, *w, *y))
+        if (!real(a[2], eps)) return nullptr;
+        if (launched([&](void* xp, void* wp, void* yp) { return abi.rmsnorm(xp, wp, yp, rows, d, (float)eps, dt, s.handle); }, *x, *w, *y))
             return given_or_new(a[3], y_new);
         return nullptr;
     });
@@ -210,14 +231,14 @@ PyObject* fast_gemm(PyObject*, PyObject* const* g, Py_ssize_t n) {
         if ((dim == 3 && b->size(0) != batch) || b->size(dim - 2) != K) return nullptr;
         if (!fits_int(batch) || !fits_int(M) || !fits_int(K) || !fits_int(N)) return nullptr;
         double slope;
-        void* st;
-        if (!real(g[2], slope) || !stream_of(g[4], *a, st)) return nullptr;
+        Where w;
+        if (!real(g[2], slope) || !stream_of(g[4], *a, w)) return nullptr;
         const int64_t shape3[3] = {batch, M, N};
         const at::IntArrayRef shape(shape3 + (3 - dim), dim);
         at::Tensor c_new;
-        if (g[3] == Py_None) c = &(c_new = new_tensor(shape, a->options()));
+        if (g[3] == Py_None) c = &(c_new = new_tensor(shape, a->options(), w));
         else if (!(c = gpu_tensor(g[3])) || c->scalar_type() != a->scalar_type() || c->sizes() != shape) return nullptr;
-        if (launched([&](void* ap, void* bp, void* cp) { return abi.gemm(ap, bp, cp, (int)batch, (int)M, (int)N, (int)K, (float)slope, dt, st); }, *a, *b, *c))
+        if (launched([&](void* ap, void* bp, void* cp) { return abi.gemm(ap, bp, cp, (int)batch, (int)M, (int)N, (int)K, (float)slope, dt, w.handle); }, *a, *b, *c))
             return given_or_new(g[3], c_new);
         return nullptr;
     });
@@ -230,7 +251,7 @@ struct NormOperands {
     long long rows;
     int d, dt;
     double eps;
-    void* st;
+    Where st;
     bool take(PyObject* px, PyObject* pr, PyObject* pw, PyObject* pe, PyObject* po, PyObject* ps) {
         x = gpu_tensor(px), w = gpu_tensor(pw);
         if (!x || !w || (dt = type_of(*x)) < 0 || x->dim() < 1 || !real(pe, eps) || !stream_of(ps, *x, st)) return false;
@@ -241,7 +262,7 @@ struct NormOperands {
         if (pr == Py_None) return true;
         auto like_x = [&](const at::Tensor* t) { return t && t->scalar_type() == x->scalar_type() && t->sizes() == x->sizes(); };
         if (!like_x(r = gpu_tensor(pr))) return false;
-        if (po == Py_None) r_out = &(r_new = new_tensor(x->sizes(), x->options()));
+        if (po == Py_None) r_out = &(r_new = new_tensor(x->sizes(), x->options(), st));
         else if (!like_x(r_out = gpu_tensor(po))) return false;
         return true;
     }
@@ -249,7 +270,7 @@ struct NormOperands {
         void *xp = x->mutable_data_ptr(), *rp = r ? r->mutable_data_ptr() : nullptr, *wp = w->mutable_data_ptr(), *yp = y.mutable_data_ptr(),
              *sp = scale ? scale->mutable_data_ptr() : nullptr, *op = r ? r_out->mutable_data_ptr() : nullptr;
         NoLock _;
-        return abi.residual_norm(xp, rp, wp, yp, (float*)sp, op, rows, d, (float)eps, dt, scale != nullptr, group, st) == 0;
+        return abi.residual_norm(xp, rp, wp, yp, (float*)sp, op, rows, d, (float)eps, dt, scale != nullptr, group, st.handle) == 0;
     }
     PyObject* r_result(PyObject* given) const { return r ? given_or_new(given, r_new) : Py_NewRef(Py_None); }
 };
@@ -273,7 +294,7 @@ PyObject* fast_residual_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
         at::Tensor y_new;
         const at::Tensor* y;
         if (!o.take(a[0], a[1], a[2], a[3], a[5], a[6])) return nullptr;
-        if (a[4] == Py_None) y = &(y_new = new_tensor(o.x->sizes(), o.x->options()));
+        if (a[4] == Py_None) y = &(y_new = new_tensor(o.x->sizes(), o.x->options(), o.st));
         else if (!(y = gpu_tensor(a[4])) || y->scalar_type() != o.x->scalar_type() || y->sizes() != o.x->sizes()) return nullptr;
         if (!o.launch(*y, nullptr, 0)) return nullptr;
         return tuple_of({given_or_new(a[4], y_new), o.r_result(a[5])});
@@ -289,11 +310,11 @@ PyObject* fast_residual_norm_fp8(PyObject*, PyObject* const* a, Py_ssize_t n) {
         if (!PyLong_CheckExact(a[4]) || !o.take(a[0], a[1], a[2], a[3], a[7], a[8])) return nullptr;
         const long group = PyLong_AsLong(a[4]);
         if (group != 0 && group != 128) return nullptr;
-        if (a[5] == Py_None) y = &(y_new = new_tensor(o.x->sizes(), o.x->options().dtype(at::kFloat8_e4m3fn)));
+        if (a[5] == Py_None) y = &(y_new = new_tensor(o.x->sizes(), o.x->options().dtype(at::kFloat8_e4m3fn), o.st));
         else if (!(y = gpu_tensor(a[5])) || y->scalar_type() != at::kFloat8_e4m3fn || y->sizes() != o.x->sizes()) return nullptr;
         c10::SmallVector<int64_t, 6> shape(o.x->sizes().begin(), o.x->sizes().end());
         shape.back() = group ? (o.d + group - 1) / group : 1;
-        if (a[6] == Py_None) s = &(s_new = new_tensor(shape, o.x->options().dtype(at::kFloat)));
+        if (a[6] == Py_None) s = &(s_new = new_tensor(shape, o.x->options().dtype(at::kFloat), o.st));
         else if (!(s = gpu_tensor(a[6])) || s->scalar_type() != at::kFloat || s->sizes() != at::IntArrayRef(shape)) return nullptr;
         if (!o.launch(*y, s, (int)group)) return nullptr;
         return tuple_of({given_or_new(a[5], y_new), given_or_new(a[6], s_new), o.r_result(a[7])});
@@ -358,8 +379,8 @@ PyObject* fast_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
             if (t->scalar_type() != type || t->size(0) != c.T || t->size(2) != c.D) return nullptr;
         if (k->size(1) != c.Hk || v->size(1) != c.Hk || !fits_int(q->size(1))) return nullptr;
         int interleaved, offset, rot = 0, angles = 0;
-        void* st;
-        if (!flag(a[10], interleaved) || !whole(a[11], offset) || !stream_of(a[13], *k, st)) return nullptr;
+        Where w;
+        if (!flag(a[10], interleaved) || !whole(a[11], offset) || !stream_of(a[13], *k, w)) return nullptr;
         if (a[8] != Py_None || a[9] != Py_None) {
             cos = gpu_tensor(a[8]), sin = gpu_tensor(a[9]);
             if (!cos || !sin || cos->scalar_type() != at::kFloat || sin->scalar_type() != at::kFloat || cos->dim() != 2 || sin->sizes() != cos->sizes()) return nullptr;
@@ -367,7 +388,7 @@ PyObject* fast_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
             angles = (int)cos->size(0), rot = 2 * (int)cos->size(1);
         }
         at::Tensor fresh;
-        if (a[12] == Py_None) out = &(fresh = new_tensor(q->sizes(), q->options()));
+        if (a[12] == Py_None) out = &(fresh = new_tensor(q->sizes(), q->options(), w));
         else if (!(out = gpu_tensor(a[12])) || out->scalar_type() != type || out->sizes() != q->sizes()) return nullptr;
         const int64_t qs = token_stride(*q), ks = token_stride(*k), vs = token_stride(*v);
         const int Hq = (int)q->size(1);
@@ -377,7 +398,7 @@ PyObject* fast_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
         int rc;
         {
             NoLock _;
-            rc = abi.append(&c, qp, kp, vp, qs, ks, vs, op, cp, sp, rot, interleaved, angles, offset, Hq, st);
+            rc = abi.append(&c, qp, kp, vp, qs, ks, vs, op, cp, sp, rot, interleaved, angles, offset, Hq, w.handle);
         }
         return rc == 0 ? given_or_new(a[12], fresh) : nullptr;
     });
@@ -391,10 +412,9 @@ PyObject* fast_paged(PyObject*, PyObject* const* a, Py_ssize_t n) {
         at::ScalarType type;
         double scale;
         int max_q, max_kv, prefix_len, want_lse;
-        void* st;
-        // another stream than the current one: a workspace of this call's own has to be told (binding.py)
-        if (!q || a[13] != Py_None || !cache_of(a + 1, q->size(0), c, type) || q->scalar_type() != type || q->size(2) != c.D || !fits_int(q->size(1))) return nullptr;
-        if (!real(a[6], scale) || !whole(a[10], prefix_len) || !flag(a[14], want_lse) || !stream_of(a[13], *q, st)) return nullptr;
+        Where w;
+        if (!q || !cache_of(a + 1, q->size(0), c, type) || q->scalar_type() != type || q->size(2) != c.D || !fits_int(q->size(1))) return nullptr;
+        if (!real(a[6], scale) || !whole(a[10], prefix_len) || !flag(a[14], want_lse) || !stream_of(a[13], *q, w)) return nullptr;
         if (a[7] == Py_None) max_q = c.T;
         else if (!whole(a[7], max_q)) return nullptr;
         if (a[8] == Py_None) {
@@ -406,16 +426,16 @@ PyObject* fast_paged(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const int Hq = (int)q->size(1);
         const int64_t sizes[3] = {c.T, Hq, c.D};
         at::Tensor o_new, lse_new, ws_new;
-        if (a[11] == Py_None) o = &(o_new = new_tensor(sizes, q->options()));
+        if (a[11] == Py_None) o = &(o_new = new_tensor(sizes, q->options(), w));
         else if (!(o = gpu_tensor(a[11])) || o->scalar_type() != type || o->sizes() != q->sizes()) return nullptr;
         if (a[12] != Py_None) {
             if (!(lse = gpu_tensor(a[12])) || lse->scalar_type() != at::kFloat || lse->sizes() != q->sizes().slice(0, 2)) return nullptr;
         } else if (want_lse) {
-            lse = &(lse_new = new_tensor(q->sizes().slice(0, 2), q->options().dtype(at::kFloat)));
+            lse = &(lse_new = new_tensor(q->sizes().slice(0, 2), q->options().dtype(at::kFloat), w));
         }
         int64_t bytes = abi.paged_workspace(c.B, c.T, Hq, c.Hk, c.D, max_q, max_kv, prefix_len);
         if (bytes < 0) return nullptr;
-        if (a[15] == Py_None) ws = &(ws_new = new_tensor(bytes, q->options().dtype(at::kByte)));
+        if (a[15] == Py_None) ws = &(ws_new = new_tensor(bytes, q->options().dtype(at::kByte), w, false));
         else if (!(ws = gpu_tensor(a[15])) || ws->scalar_type() != at::kByte) return nullptr;
         bytes = ws->numel();
         const void *qp = q->mutable_data_ptr(), *pp = prefix ? prefix->mutable_data_ptr() : nullptr;
@@ -425,7 +445,7 @@ PyObject* fast_paged(PyObject*, PyObject* const* a, Py_ssize_t n) {
         int rc;
         {
             NoLock _;
-            rc = abi.paged(&c, qp, qs, op, lp, (const int*)pp, prefix_len, Hq, max_q, max_kv, (float)scale, wp, bytes, st);
+            rc = abi.paged(&c, qp, qs, op, lp, (const int*)pp, prefix_len, Hq, max_q, max_kv, (float)scale, wp, bytes, w.handle);
         }
         if (rc != 0) return nullptr;
         return tuple_of({given_or_new(a[11], o_new), lse_new.defined() ? THPVariable_Wrap(lse_new) : Py_NewRef(a[12])});
