@@ -76,6 +76,7 @@ inline int paged_block_keys(int rows, int D) { return rows < 128 && D == 128 ? 3
 inline PagedPlan paged_plan(int B, int T, int Hq, int Hk, int D, int max_q, int max_kv, int prefix_len) {
     PagedPlan p{};
     const int G = Hq / Hk;
+    max_q = max_q < T ? max_q : T;   // (a hint may be any number; no sequence has more new tokens than there are)
     p.rows = paged_rows((long long)max_q * G);
     const int R = p.rows, KB = paged_block_keys(R, D);
     // tiles of rows: of every sequence at most, and of all its tokens together
@@ -85,9 +86,10 @@ inline PagedPlan paged_plan(int B, int T, int Hq, int Hk, int D, int max_q, int 
     // of 512 keys, 32 / 8 heads, D = 128: 9.9 us whole, 11.2 shared out; of 1024: 15.3 and 11.2, with four wavefronts; of 512 with eight
     // 7.0 us whole), less so where there are more tiles
     // than compute units (64 sequences of 1 to 1024 keys: 16.8 and 21.4; 256 of 100 to 2048: 135 and 140; 16 of 1 to 2048: 26 and 19).
-    // (Work is counted in 32 bits, of max_kv keys a tile at most: whatever may be past 2^31 blocks has tiles enough.)
+    // (Work is counted in 32 bits, of max_kv keys a tile at most: whatever may be past 2^31 blocks has tiles enough.  A division: the product with a
+    // hint of 2^31 - 1 keys may pass 64 bits.)
     const long long often = segments / 256;
-    p.balanced = max_kv > 16 * KB * (often < 1 ? 1 : often > 4 ? 4 : often) && each * Hk * (max_kv / KB + 64) < (1LL << 31);
+    p.balanced = max_kv > 16 * KB * (often < 1 ? 1 : often > 4 ? 4 : often) && each * Hk <= ((1LL << 31) - 1) / (max_kv / KB + 64);
     p.direct = !p.balanced && (long long)max_q * G <= R;
     // Eight wavefronts where a workgroup has a compute unit for itself: whole tiles take half the rounds (one sequence of 512 keys 8.8 us,
     // 10.1 with four), shared-out ones have half the parts, if there is work for all (65537 keys 57 and 61; 4 sequences of 4096 20.2 and

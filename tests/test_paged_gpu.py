@@ -190,6 +190,16 @@ def test_a_hint_that_is_too_small(D, Hq, Hk):
         check(attend(s, D ** -0.5, max_kv=hint), ref, BF16)
 
 
+def test_hints_that_are_far_too_large():
+    s = make([1, 2, 1, 3], [300, 120, 5, 0], 8, 2, 64, 16, F16, prefix=40, seed=21)
+    ref, top = reference(s, 0.125), 2 ** 31 - 1
+    for max_kv in (300, 5000, top):
+        want = attend(s, 0.125, max_q=7, max_kv=max_kv)
+        check(want, ref, F16)
+        got = attend(s, 0.125, max_q=top, max_kv=max_kv)
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
 @pytest.mark.parametrize("rising", [True, False])
 def test_many_rows_whose_references_move(rising):
     """128-row tiles: keys whose logits rise or fall all along the sequence, a row's own limit inside the last blocks."""

@@ -135,3 +135,22 @@ def test_a_key_s_place_in_a_page_of_any_size(L, D):
         size = 1 << shift
         for j in {0, 1, size // 2, size - 1, size, (1 << 23) - 1, 1 << 23, (1 << 23) + 77, 1 << 24, (1 << 30) - 1}:
             assert L.key_offset(j, size - 1, 2 * D) == j % size * 2 * D, (shift, j)
+
+
+def test_hints_of_any_size(L):
+    """max_q and max_kv are hints, any number that an int holds: work that is shared out fits 32 bits all the same, and more new tokens than there are
+    count as all of them."""
+    top = 2 ** 31 - 1
+    r = random.Random(8)
+    sizes = [(256, 256, 64, 8, 128), (1, 1, 8, 8, 64), (1 << 20, 1 << 20, 4, 4, 128), (1, 1 << 22, 64, 1, 128), (4096, 1 << 20, 128, 16, 64)]
+    sizes += [(r.choice([1, 3, 64, 5000]), r.choice([1, 64, 4096, 100000]), 8 * r.choice([1, 4, 16]), r.choice([1, 2, 8]), r.choice([32, 64, 128])) for _ in range(300)]
+    for B, T, Hq, Hk, D in sizes:
+        for max_q in (1, T, top // 3, top):
+            for max_kv in (0, 5000, 1 << 20, top - 1, top):
+                p = plan(L, B, T, Hq, Hk, D, max_q, max_kv, 0)
+                assert p == plan(L, B, T, Hq, Hk, D, min(max_q, T), max_kv, 0), (B, T, Hq, Hk, D, max_q, max_kv)
+                assert 0 <= p["bytes"] == P.attn_paged_workspace(B, T, Hq, Hk, D, max_q, max_kv, 0)
+                if p["balanced"]:
+                    KB = 32 if p["rows"] < 128 and D == 128 else 64
+                    tiles = B * -(-min(max_q, T) * (Hq // Hk) // p["rows"]) * Hk
+                    assert tiles * (max_kv // KB + 9) < 2 ** 31, (B, T, Hq, Hk, D, max_q, max_kv)
