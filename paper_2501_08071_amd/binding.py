@@ -135,6 +135,14 @@ def _new(shape, dtype, device, stream, returned=True):
     return t
 
 
+def _int32(x, name: str) -> int:
+    """x as the C call takes it (ctypes would drop what lies above 32 bits without a word)."""
+    x = int(x)
+    if not -2 ** 31 <= x < 2 ** 31:
+        raise ValueError(f"{name} must fit 32 bits")
+    return x
+
+
 def attn_status_str(status: int) -> str:
     return lib.attn_status_str(int(status)).decode()
 
@@ -328,7 +336,8 @@ def attn_fwd(q, k, v, causal: bool, scale: float, o=None, lse=None, stream=None,
 
 def attn_paged_workspace(B: int, T: int, Hq: int, Hk: int, D: int, max_q: int, max_kv: int, prefix_len: int = 0) -> int:
     """Bytes of workspace attn_paged_fwd needs for these sizes (-1: sizes it refuses)."""
-    return int(lib.attn_paged_workspace(int(B), int(T), int(Hq), int(Hk), int(D), int(max_q), int(max_kv), int(prefix_len)))
+    sizes = [int(n) for n in (B, T, Hq, Hk, D, max_q, max_kv, prefix_len)]
+    return int(lib.attn_paged_workspace(*sizes)) if all(-2 ** 31 <= n < 2 ** 31 for n in sizes) else -1
 
 
 def attn_kv_append_raw(cache: PagedCache, q_ptr, k_ptr, v_ptr, q_stride, k_stride, v_stride, q_out_ptr, cos_ptr, sin_ptr, rot, interleaved,
@@ -377,7 +386,8 @@ def _paged_cache(k_cache, v_cache, page_table, cu_q, kv_len, T) -> PagedCache:
     B = kv_len.shape[0] if kv_len.dim() == 1 else -1
     _ints(kv_len, "kv_len", (None,)), _ints(cu_q, "cu_q", (B + 1,)), _ints(page_table, "page_table", (B, None))
     return PagedCache(k_cache.data_ptr() or None, v_cache.data_ptr() or None, k_cache.stride(0) if n_pages > 1 else Hk * page * D, n_pages, page, Hk, D,
-                      dtype, page_table.data_ptr() or None, page_table.stride(0) if B > 1 else page_table.shape[1], page_table.shape[1],
+                      dtype, page_table.data_ptr() or None,
+                      _int32(page_table.stride(0), "page_table's stride") if B > 1 else page_table.shape[1], page_table.shape[1],
                       cu_q.data_ptr() or None, kv_len.data_ptr() or None, B, T)
 
 
@@ -420,6 +430,7 @@ def attn_kv_append(q, k, v, k_cache, v_cache, page_table, cu_q, kv_len, cos=None
         if cos.dim() != 2 or sin.shape != cos.shape or not cos.is_cuda or not sin.is_cuda or not cos.is_contiguous() or not sin.is_contiguous():
             raise ValueError("cos and sin must be contiguous device tensors [positions, rot / 2] of one shape")
         n_angles, rot = cos.shape[0], 2 * cos.shape[1]
+    pos_offset = _int32(pos_offset, "pos_offset")
     st = (stream or torch.cuda.current_stream(k.device)).cuda_stream
     ptr = lambda t: t.data_ptr() if t is not None else 0  # noqa: E731
     rc = attn_kv_append_raw(cache, ptr(q), ptr(k), ptr(v), qs, ks, vs, ptr(q_out), ptr(cos), ptr(sin), rot, bool(interleaved), n_angles,
@@ -452,10 +463,11 @@ def attn_paged_fwd(q, k_cache, v_cache, page_table, cu_q, kv_len, scale: float, 
     qs, Hq = _heads(q, "q", T, D), q.shape[1]
     if cache.Hk == 0 or Hq == 0 or Hq % cache.Hk:
         raise ValueError("the heads of q must be a multiple of the cache's")
-    max_q = T if max_q is None else int(max_q)
-    max_kv = cache.width * cache.page_size if max_kv is None else int(max_kv)
+    max_q = T if max_q is None else _int32(max_q, "max_q")
+    max_kv = min(cache.width * cache.page_size, 2 ** 31 - 1) if max_kv is None else _int32(max_kv, "max_kv")
+    prefix_len = _int32(prefix_len, "prefix_len")
     if prefix_len:
-        need = -(-int(prefix_len) // max(1, cache.page_size))
+        need = -(-prefix_len // max(1, cache.page_size))
         if prefix_table is None or prefix_table.dim() != 1 or prefix_table.shape[0] < need:
             raise ValueError("prefix_table must hold the pages of prefix_len keys")
         _ints(prefix_table, "prefix_table", (None,))
@@ -559,6 +571,7 @@ def residual_rmsnorm_fwd_raw(x_ptr, r_ptr, w_ptr, y_ptr, scale_ptr, r_out_ptr, n
 
 
 def _residual_norm(x, r, w, eps, fp8, group, y, scale, r_out, stream):
+    group = _int32(group, "group")
     dtype, y16, n_rows, n = _row_args(x, x if fp8 else y, stream)
     if w.dtype != x.dtype or tuple(w.shape) != (n,) or not w.is_cuda or not w.is_contiguous():
         raise ValueError("w must be a contiguous device tensor [d] of x's dtype")
@@ -576,7 +589,7 @@ def _residual_norm(x, r, w, eps, fp8, group, y, scale, r_out, stream):
     if fp8:
         if y.dtype != torch.float8_e4m3fn or y.shape != x.shape or not y.is_cuda or not y.is_contiguous():
             raise ValueError("y must be a contiguous float8_e4m3fn device tensor of the shape of x")
-        shape = (*x.shape[:-1], -(-n // int(group)) if group else 1)
+        shape = (*x.shape[:-1], -(-n // group) if group else 1)
         if scale is None:
             scale = _new(shape, torch.float32, x.device, stream)
         elif scale.dtype != torch.float32 or scale.shape != shape or not scale.is_cuda or not scale.is_contiguous():

@@ -528,3 +528,18 @@ def test_both_ways_agree_and_what_is_refused(way):
     with pytest.raises(P.AttnError):
         fwd(kc=page3, vc=page3)
     torch.cuda.synchronize()
+
+
+def test_numbers_past_32_bits_are_refused(way):
+    s = make([1, 3], [40, 90], 4, 2, 64, 16, F16, prefix=20, seed=1)
+    k, v = (torch.randn(4, 2, 64, device="cuda").to(F16) for _ in range(2))
+    cos = torch.ones(200, 32, device="cuda")
+    for far in (2 ** 32, 2 ** 32 + 3, -2 ** 32 + 3, 2 ** 31, 2 ** 40):
+        for x in ("max_q", "max_kv"):
+            with pytest.raises(ValueError):
+                attend(s, 0.125, **{x: far})
+        with pytest.raises(ValueError):
+            attend({**s, "prefix_len": far}, 0.125)
+        with pytest.raises(ValueError):
+            P.attn_kv_append(s["q"], k, v, s["k_cache"], s["v_cache"], s["page_table"], s["cu_q"], s["kv_len"], cos=cos, sin=cos, pos_offset=far)
+    torch.cuda.synchronize()

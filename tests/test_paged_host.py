@@ -154,3 +154,11 @@ def test_hints_of_any_size(L):
                     KB = 32 if p["rows"] < 128 and D == 128 else 64
                     tiles = B * -(-min(max_q, T) * (Hq // Hk) // p["rows"]) * Hk
                     assert tiles * (max_kv // KB + 9) < 2 ** 31, (B, T, Hq, Hk, D, max_q, max_kv)
+
+
+def test_sizes_past_32_bits_have_no_workspace():
+    good = [2, 3, 16, 8, 64, 2, 100000, 77]
+    assert P.attn_paged_workspace(*good) > 0
+    for i in range(8):
+        for far in (2 ** 32, -2 ** 32, 2 ** 31, -2 ** 31 - 1):
+            assert P.attn_paged_workspace(*good[:i], good[i] + far, *good[i + 1:]) == -1, (i, far)

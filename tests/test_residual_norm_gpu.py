@@ -163,3 +163,11 @@ def test_both_ways_agree_and_what_is_refused(way):
         with pytest.raises(kind):
             call()
     torch.cuda.synchronize()
+
+
+def test_a_group_past_32_bits_is_refused(way):
+    x, r, w = make(6, 300, torch.float16)
+    for group in (2 ** 32, 2 ** 32 + 128, -2 ** 32, 2 ** 40):
+        with pytest.raises(ValueError):
+            P.residual_rmsnorm_fwd_fp8(x, r, w, EPS, group=group)
+    torch.cuda.synchronize()
