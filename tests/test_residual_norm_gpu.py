@@ -79,6 +79,28 @@ def test_more_rows_than_a_grid_holds(rows, d):
     check_fp8(y8, scale, ref, 128)
 
 
+# 1024 threads a row: 512 workgroups at most; rows past 32768 elements: read twice; short rows: 32 to a workgroup, 2^22 workgroups at most
+@pytest.mark.parametrize("rows,d,dtype", [(1100, 16392, torch.bfloat16), (1100, 16389, torch.float16), (1537, 32768, torch.float16), (1100, 32776, torch.bfloat16),
+                                          (1537, 32771, torch.float16), (2 ** 27 + 1000, 1, torch.bfloat16), (2 ** 27 + 1000, 8, torch.float16)])
+def test_a_workgroup_goes_round_the_rows(rows, d, dtype):
+    """More rows than a launch has places for them: the second and third of a workgroup are as right as its first."""
+    x, r, w = make(rows, d, dtype, seed=d)
+    size = rows * d
+    buf = torch.full((size + 16,), 7.0, dtype=dtype, device="cuda")
+    y, r_out = P.residual_rmsnorm_fwd(x, r, w, EPS, y=buf[8:8 + size].view(rows, d))
+    eight = [(group, P.residual_rmsnorm_fwd_fp8(x, r, w, EPS, group=group)) for group in (0, 128)]
+    assert (buf[:8] == 7.0).all() and (buf[8 + size:] == 7.0).all()
+    step = max(1, 2 ** 26 // d)
+    for a in range(0, rows, step):
+        part = slice(a, a + step)
+        h, ref = formula(x[part], r[part], w)
+        assert near(y[part], ref, dtype)
+        assert ((r_out[part].double() - h).abs() <= (U[dtype] + 2.0 ** -23) * h.abs() + 2.0 ** -25).all()
+        for group, (y8, scale, r8) in eight:
+            check_fp8(y8[part], scale[part], ref, group)
+            assert torch.equal(r8[part], r_out[part])
+
+
 @pytest.mark.parametrize("d", [65, 512, 4099, 16384, 40000])
 def test_in_place(d):
     """The residual updated in its own buffer, y over x."""
