@@ -716,9 +716,10 @@ __device__ __forceinline__ void leave(const PagedAttnLaunch& a, const Prefix& px
     if (d == 0) *(f32x2*)(const_cast<float*>(px.ml) + 2 * at) = f32x2{m, l};
 }
 
-template <int DTY, int D, int RT, int NW>
-__global__ __launch_bounds__(64 * NW, 2) void attn_paged_prefix_kernel(PagedAttnLaunch a, Prefix px) {
+template <int DTY, int D, int RT>
+__global__ __launch_bounds__(64 * NARROW_PREFIX_WAVES, 2) void attn_paged_prefix_kernel(PagedAttnLaunch a, Prefix px) {
     using S = Shape<D>;
+    constexpr int NW = NARROW_PREFIX_WAVES;
     __shared__ __align__(16) char lds[NW * S::BUF];
     __shared__ float ml[NW][16][2];
     int split, from, to;
@@ -1023,10 +1024,8 @@ hipError_t launch(const PagedAttnLaunch& a) {
     const long long rows = (long long)a.c.T * a.Hq;
     Prefix px{ws, ws + p.prefix_splits * rows * D, p.prefix_splits, rows};
     if (p.prefix_splits > 0) {
-        const bool w8 = p.prefix_waves == 8;
-        auto kernel = p.prefix_rows == 16 ? (w8 ? &attn_paged_prefix_kernel<DTY, D, 1, 8> : &attn_paged_prefix_kernel<DTY, D, 1, 4>)
-                      : p.prefix_rows == 32 ? (w8 ? &attn_paged_prefix_kernel<DTY, D, 2, 8> : &attn_paged_prefix_kernel<DTY, D, 2, 4>)
-                                            : &attn_paged_wide_prefix_kernel<DTY, D>;
+        auto kernel = p.prefix_rows == 16 ? &attn_paged_prefix_kernel<DTY, D, 1>
+                      : p.prefix_rows == 32 ? &attn_paged_prefix_kernel<DTY, D, 2> : &attn_paged_wide_prefix_kernel<DTY, D>;
         const hipError_t e = start(kernel, dim3(p.prefix_tiles * a.c.Hk * p.prefix_splits), 64 * p.prefix_waves, a.stream, a, px);
         if (e != hipSuccess) return e;
     }

@@ -69,6 +69,7 @@ struct PagedPlan {
     long long part_floats, prefix_floats, bytes;         // workspace: parts of split tiles, results of the prefix pass, all of it
 };
 constexpr int PAGED_WAVES = 2048;   // eight to a compute unit: what their LDS allows
+constexpr int NARROW_PREFIX_WAVES = 8;   // of a workgroup of 16 or 32 rows in the pass over a shared prefix: few rows have few tiles
 
 inline int paged_rows(long long rows) { return rows <= 16 ? 16 : rows <= 32 ? 32 : 128; }
 inline int paged_block_keys(int rows, int D) { return rows < 128 && D == 128 ? 32 : 64; }
@@ -109,7 +110,7 @@ inline PagedPlan paged_plan(int B, int T, int Hq, int Hk, int D, int max_q, int 
         const long long least = R < 128 ? 2 : 4, cap = R < 128 ? 16 : 4, fine = (blocks + least - 1) / least;
         long long most = (blocks + 7) / 8;
         if (PR == 128 && most < cap) most = fine < cap ? fine : cap;
-        p.prefix_waves = PR < 128 ? 8 : 4;
+        p.prefix_waves = PR < 128 ? NARROW_PREFIX_WAVES : 4;
         long long s = PAGED_WAVES / p.prefix_waves / groups;
         s = s > most ? most : s > top ? top : s;
         s = s < 1 ? 1 : s;
