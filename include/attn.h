@@ -29,13 +29,15 @@ typedef enum { ATTN_F16 = 0, ATTN_BF16 = 1 } attn_dtype_t;
 
 typedef enum {
     ATTN_OK = 0,
-    ATTN_ERR_NULL = -1,        /* q, k, v or o is NULL                               */
-    ATTN_ERR_SHAPE = -2,       /* B, H, S or D <= 0, or a tensor above 2^40 elements */
+    ATTN_ERR_NULL = -1,        /* a tensor that the call needs is NULL               */
+    ATTN_ERR_SHAPE = -2,       /* B, H, S or D <= 0, or a tensor above 2^40 elements;
+                                  on a paged cache: sizes out of the limits below    */
     ATTN_ERR_DTYPE = -3,       /* dtype is not an attn_dtype_t                       */
     ATTN_ERR_SCALE = -4,       /* scale is NaN or infinite                           */
     ATTN_ERR_UNSUPPORTED = -5, /* valid request with no kernel instance (D)          */
     ATTN_ERR_LAUNCH = -6,      /* the HIP runtime refused the launch                 */
-    ATTN_ERR_ALIGN = -7,       /* a pointer is not 16-byte aligned                   */
+    ATTN_ERR_ALIGN = -7,       /* a pointer is not 16-byte aligned (on a paged cache
+                                  pointers to int, and lse: 4-byte)                  */
     ATTN_ERR_WORKSPACE = -8    /* attn_paged_fwd: the workspace is missing or small  */
 } attn_status_t;
 
@@ -132,6 +134,9 @@ int attn_workgroup_rows(int B, int H, int S, int D, int dtype, int causal);
  *   cu_q         DEVICE pointer, [B + 1]: the new tokens of sequence b are rows cu_q[b] .. cu_q[b + 1] - 1.  May be none.
  *   kv_len       DEVICE pointer, [B]: keys of the sequence in its pages, the new tokens' among them.
  *   page_size    a power of two.      D: 32, 64 or 128.      Hk: key heads.
+ *
+ * Limits: B <= 2^20, T <= 2^22, T times the larger of Hq and Hk <= 2^28, B * Hk <= 2^22, width * page_size <= 2^30 keys a sequence,
+ * page_stride * n_pages <= 2^40 elements; with T and B not 0, n_pages at least 1.
  *
  * Values on the device cannot be checked by the host.  Whatever they are, nothing outside the buffers is touched: a page number
  * outside 0 .. n_pages - 1 is a page of absent keys, lengths are cut to the table's width, rows to T.

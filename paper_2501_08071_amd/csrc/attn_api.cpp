@@ -21,12 +21,14 @@ extern "C" int attn_supported(int S, int D, int dtype, int causal) {
 extern "C" const char* attn_status_str(int status) {
     switch (status) {
         case ATTN_OK: return "ok";
-        case ATTN_ERR_NULL: return "q, k, v or o is a null pointer";
-        case ATTN_ERR_SHAPE: return "B, H, S and D must be positive (and a tensor at most 2^40 elements)";
+        case ATTN_ERR_NULL: return "q, k, v or o (on a paged cache: or the page table, cu_q, kv_len, the prefix's table, q_out, cos or sin) is a null pointer";
+        case ATTN_ERR_SHAPE: 
+            return "B, H, S and D must be positive and a tensor at most 2^40 elements (on a paged cache: page_size a power of two, pages and tokens "
+                   "multiples of 8 elements apart, Hq a multiple of Hk, rot a multiple of 16 up to D, lengths and sizes within the limits of attn.h)";
         case ATTN_ERR_DTYPE: return "dtype must be ATTN_F16 (0) or ATTN_BF16 (1)";
         case ATTN_ERR_SCALE: return "scale must be finite";
         case ATTN_ERR_UNSUPPORTED: return "no kernel instance for this head dimension (D must be 32, 64 or 128)";
-        case ATTN_ERR_ALIGN: return "every pointer must be 16-byte aligned";
+        case ATTN_ERR_ALIGN: return "every pointer must be 16-byte aligned (on a paged cache those to int, and lse: 4-byte)";
         case ATTN_ERR_LAUNCH: return "the HIP runtime refused the kernel launch";
         case ATTN_ERR_WORKSPACE: return "the workspace is missing or smaller than attn_paged_workspace says";
         default: return "unknown status";

@@ -162,3 +162,16 @@ def test_sizes_past_32_bits_have_no_workspace():
     for i in range(8):
         for far in (2 ** 32, -2 ** 32, 2 ** 31, -2 ** 31 - 1):
             assert P.attn_paged_workspace(*good[:i], good[i] + far, *good[i + 1:]) == -1, (i, far)
+
+
+def test_a_refusal_says_what_may_be_wrong_on_a_paged_cache():
+    say = lambda status: P.lib.attn_status_str(status).decode()  # noqa: E731
+    assert fwd(cache(page_size=24)) == -2 and "page_size a power of two" in say(-2)
+    assert fwd(Hq=12) == -2 and "Hq a multiple of Hk" in say(-2) and append(rot=24) == -2 and "rot a multiple of 16" in say(-2)
+    assert fwd(cache(kv_len=None)) == -1 and "kv_len" in say(-1) and append(cos=0) == -1 and "cos" in say(-1)
+    assert fwd(lse=OK + 2) == -7 and fwd(lse=OK + 4) != -7 and "4-byte" in say(-7)
+    # the limits that the header names: at them, and past them
+    for at, past in ((dict(B=1 << 18, Hk=16, page_stride=1 << 20), dict(B=1 << 18, Hk=32, page_stride=1 << 20)), (dict(T=1 << 22), dict(T=(1 << 22) + 1)), (dict(width=1 << 26, table_stride=1 << 26), dict(width=(1 << 26) + 1, table_stride=1 << 27)),
+                     (dict(n_pages=1 << 10, page_stride=1 << 30), dict(n_pages=1 << 10, page_stride=(1 << 30) + 8))):
+        stop = dict(k=None)        # (a null pointer is found after the sizes: nothing is launched)
+        assert append(cache(**at, **stop), q=0, Hq=0) == -1 and append(cache(**past, **stop), q=0, Hq=0) == -2, (at, past)
