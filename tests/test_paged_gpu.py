@@ -324,6 +324,20 @@ def test_what_non_finite_values_do():
     assert torch.equal(again.view(torch.int16), o.view(torch.int16))
 
 
+@pytest.mark.parametrize("n,bad", [(5, 3), (70, 40)])       # 16- and 128-row tiles
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf")])
+def test_a_key_that_a_row_does_not_see_may_hold_anything(n, bad, value):
+    """A new token's key that is not finite: the tokens before it are as right as without."""
+    for D, dtype in ((64, F16), (128, BF16)):
+        s = make([n], [n + 30], 2, 1, D, 16, dtype, seed=n)
+        ref, at = reference(s, 0.125), 30 + bad
+        s["k_cache"][s["page_table"][0, at // 16].long(), 0, at % 16] = value
+        for max_kv in (n + 30, 1 << 20):
+            o, lse = attend(s, 0.125, max_kv=max_kv)
+            check((o[:bad], lse[:bad]), tuple(t[:bad] for t in ref), dtype)
+            assert value == value or (torch.isnan(o[bad:]).all() and torch.isnan(lse[bad:]).all())
+
+
 def test_pages_that_do_not_exist_are_absent_keys():
     s = make([1], [160], 2, 1, 64, 16, F16, seed=2)
     t = s["page_table"]
