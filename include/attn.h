@@ -80,7 +80,7 @@ int attn_fwd(const void *q, const void *k, const void *v, float *o, float *lse,
  * The same operation with O written in the type of q, k and v (Table 2 gives the kernel's inputs as
  * fp16 tensors; a layer that feeds the next one in half precision wants O that way), rounded to
  * nearest even from the fp32 result (so its error is that of attn_fwd plus one rounding of O: at most
- * 2^-9 |O| for bfloat16, 2^-12 |O| for binary16).  `o` is [B,H,S,D] contiguous in `dtype`; lse stays fp32.  Every
+ * 2^-8 |O| for bfloat16, 2^-11 |O| for binary16).  `o` is [B,H,S,D] contiguous in `dtype`; lse stays fp32.  Every
  * other argument, the ownership and error rules are those of attn_fwd; both share one kernel.
  */
 int attn_fwd_o16(const void *q, const void *k, const void *v, void *o, float *lse,
@@ -183,12 +183,18 @@ int attn_kv_append(const attn_paged_t *cache, const void *q, const void *k, cons
  *   lse          DEVICE pointer, [T][Hq] fp32, or NULL.
  *   prefix_table DEVICE pointer, the pages of a prefix that all sequences share, or NULL with prefix_len 0.  Its keys are read once
  *                for all of the batch's rows that fit a tile, not once a sequence.
- *   max_q        the most new tokens any sequence has; rows past it, and rows that no sequence owns, are not written.
+ *   max_q        the most new tokens any sequence has; rows past it, and rows that no sequence owns, are not written.  It chooses the kernel:
+ *                a number that is too large costs speed (a decode step told of T new tokens a sequence may take twice as long).
  *   max_kv       the most keys of its own any sequence has: only a hint of how to share out the work.
  *   workspace    DEVICE pointer of attn_paged_workspace(...) bytes (16-byte aligned) that no other call uses meanwhile; NULL where that is 0.
  *
- * Keys and values that only some rows of a sequence's new tokens see must be finite for the others too (a hidden one has weight 0,
- * and 0 * Inf is not 0); slots past kv_len may hold anything.  Runs repeat bit for bit.  Else as attn_fwd.
+ * Logits, statistics and sums are fp32.  Two roundings to `dtype`: of the weights exp(s_j - reference) before they meet the values (their sum is taken
+ * before it), and of o.  With u = 2^-8 for bfloat16 and 2^-11 for binary16 they move o by up to u sum_j p_j |v_j| + u |o|, p_j the share of
+ * key j (binary16 weights below 2^-14 also lose up to 2^-25 each); against 64 bits the error is measured at 1.2 to 1.4 times that of an evaluation
+ * in fp32 that is rounded once.
+ *
+ * Values that only some rows of a sequence's new tokens see must be finite for the others too (a hidden one has weight 0,
+ * and 0 * Inf is not 0).  Keys that a row does not see, and slots past kv_len, may hold anything.  Runs repeat bit for bit.  Else as attn_fwd.
  */
 int attn_paged_fwd(const attn_paged_t *cache, const void *q, long long q_stride, void *o, float *lse,
                    const int *prefix_table, int prefix_len, int Hq, int max_q, int max_kv, float scale,

@@ -74,7 +74,8 @@ int rmsnorm_fwd(const void* x, const void* w, void* y, long long n_rows, int d, 
  *     h = x + r,   r_out = h,   y[i,j] = h[i,j] / sqrt(mean_j' h[i,j']^2 + eps) * w[j]
  *     8 bits:  scale = max |y| / 448 over the row, or over each 128 columns of it (1 where every y is 0),  y8 = e4m3(y / scale)
  *
- * h stays fp32 between the addition and the results, which are rounded to nearest even.  e4m3 is the OCP 8-bit type (1, 4, 3 bits, no
+ * h stays fp32 between the addition and the results, which are rounded to nearest even, and so does the sum of squares: where it passes fp32's range
+ * (bfloat16 values near 2^63) a row's y is 0.  e4m3 is the OCP 8-bit type (1, 4, 3 bits, no
  * infinity, largest value 448).  A row with a NaN or an infinity gives NaN where the formulas do, its scale included.
  *
  *   x, r     DEVICE pointers, [n_rows, d] contiguous, elements of `dtype`.  r may be NULL: h = x, and r_out is not used.
@@ -84,7 +85,7 @@ int rmsnorm_fwd(const void* x, const void* w, void* y, long long n_rows, int d, 
  *   r_out    DEVICE pointer, [n_rows, d] contiguous, elements of `dtype`.  Written.  May be r or x, not y.
  *   group    0 or 128 (without fp8: 0).
  *   n_rows, d, eps, dtype, stream, ownership, errors: as above; a group of another size is ROWOPS_ERR_SHAPE.  A row of up to 32768
- *            elements is read once, a longer one twice.  With fp8 every h * w must be finite in fp32.
+ *            elements is read once, a longer one twice and two to four times as slowly.  With fp8 every h * w must be finite in fp32.
  */
 int residual_rmsnorm_fwd(const void* x, const void* r, const void* w, void* y, float* scale, void* r_out, long long n_rows, int d,
                          float eps, int dtype, int fp8, int group, void* stream);

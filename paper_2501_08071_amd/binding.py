@@ -446,7 +446,9 @@ def attn_paged_fwd(q, k_cache, v_cache, page_table, cu_q, kv_len, scale: float, 
 
     q                : [T, Hq, D], a token's heads contiguous; Hq a multiple of the cache's Hk.
     k_cache, v_cache, page_table, cu_q, kv_len : as for attn_kv_append.
-    max_q            : the most new tokens any sequence has (default T); max_kv: the most own keys (a hint; default what the table holds).
+    max_q            : the most new tokens any sequence has (default T, which is safe, and slow for a decode step: 64 sequences of 1 to 1024 keys take 29 us
+                       with it and 14.5 with 1); rows past it, and rows that no sequence owns, are not written.
+    max_kv           : the most own keys (a hint of how to share out the work; default what the table holds).
     prefix_table, prefix_len : int32 pages of a prefix in front of every sequence, and its length.
     o, lse           : optional preallocated outputs [T, Hq, D] of q's dtype, [T, Hq] fp32.
     workspace        : optional uint8 tensor of attn_paged_workspace(...) bytes; allocated for the call if None.

@@ -29,8 +29,9 @@ struct AppendLaunch {
 };
 hipError_t kv_append_launch(const AppendLaunch& a);
 
-// n / d for 0 <= n < 2^31 as a product: with 2^(l-1) < d <= 2^l and m = floor(2^(31+l) / d) + 1 < 2^32 + 1, n m / 2^(31+l) exceeds n / d by less
-// than n / 2^31 / d < 1 / d.  (A division by a number that is not known in advance takes 40 instructions; a small problem waits for several.)
+// n / d for 0 <= n < 2^31 as a product: with 2^(l-1) < d <= 2^l and m = floor(2^(31+l) / d) + 1, n m / 2^(31+l) exceeds n / d by less
+// than n / 2^31 / d < 1 / d.  m has 32 bits: for d = 2^l it is 2^31 + 1, else d is 2^(l-1) + 1 or more, 2^(31+l) / d at most
+// 2^32 - 2^32 / (2^(l-1) + 1), and with d < 2^31 that is below 2^32 - 3.  (A division by a number that is not known in advance takes 40 instructions; a small problem waits for several.)
 struct Divisor {
     uint32_t m = 1, shift = 0;
     Divisor() = default;
@@ -83,19 +84,26 @@ inline PagedPlan paged_plan(int B, int T, int Hq, int Hk, int D, int max_q, int 
     // tiles of rows: of every sequence at most, and of all its tokens together
     const long long each = (long long)B * (((long long)max_q * G + R - 1) / R), all = (long long)T * G / R + B;
     const long long segments = (each < all ? each : all) * Hk;
-    // Whole tiles while they are short: sharing out costs a scan, sums through memory and a second launch (a decode step of one sequence
-    // of 512 keys, 32 / 8 heads, D = 128: 9.9 us whole, 11.2 shared out; of 1024: 15.3 and 11.2, with four wavefronts; of 512 with eight
-    // 7.0 us whole), less so where there are more tiles
-    // than compute units (64 sequences of 1 to 1024 keys: 16.8 and 21.4; 256 of 100 to 2048: 135 and 140; 16 of 1 to 2048: 26 and 19).
+    // Whole tiles while they are short: sharing out costs a scan, sums through memory and a second launch, less so where there are more
+    // tiles than compute units.  Decode steps, 32 / 8 heads, D = 128, bfloat16, us a call on the same inputs again and again, the four ways (this rule
+    // and the next one) in one run:
+    //                                            whole, 4 wavefronts   whole, 8   shared out, 4   shared out, 8   chosen
+    //     1 sequence of 512 keys                         8.4              7.1         11.6            14.4        whole, 8
+    //     1 of 1024                                     13.1              9.8         11.9            14.6        shared out, 4 (the second best)
+    //     2 of 2048                                     22.8             16.0         12.7            15.1        shared out, 4
+    //     4 of 4096                                     42.0             28.2         21.0            18.9        shared out, 8
+    //     1 of 65537                                     612              377         50.5            48.4        shared out, 8
+    //     16 of 1 to 2048                               22.9             16.1         17.5            17.6        shared out (the second best)
+    //     64 of 1 to 1024                               14.7             15.3         22.3            26.8        whole, 4
+    //     256 of 100 to 2048                             130              131          142             151        whole, 4
+    //     64 of 200 to 8192                              140              136          110             112        shared out, 4
     // (Work is counted in 32 bits, of max_kv keys a tile at most: whatever may be past 2^31 blocks has tiles enough.  A division: the product with a
     // hint of 2^31 - 1 keys may pass 64 bits.)
     const long long often = segments / 256;
     p.balanced = max_kv > 16 * KB * (often < 1 ? 1 : often > 4 ? 4 : often) && each * Hk <= ((1LL << 31) - 1) / (max_kv / KB + 64);
     p.direct = !p.balanced && (long long)max_q * G <= R;
-    // Eight wavefronts where a workgroup has a compute unit for itself: whole tiles take half the rounds (one sequence of 512 keys 8.8 us,
-    // 10.1 with four), shared-out ones have half the parts, if there is work for all (65537 keys 57 and 61; 4 sequences of 4096 20.2 and
-    // 22.7; 2 of 2048 15.4 and 14.2), and two workgroups of four hide each other's ends where there are many tiles (64 sequences of 200
-    // to 8192 133 and 131).
+    // Eight wavefronts where a workgroup has a compute unit for itself: whole tiles take half the rounds, shared-out ones have half the parts,
+    // if there is work for all, and two workgroups of four hide each other's ends where there are many tiles (figures: the table above).
     p.waves = R < 128 && segments <= 256 && (!p.balanced || segments * (max_kv / KB) >= 2048) ? 8 : 4;
     p.workgroups = p.balanced ? PAGED_WAVES / p.waves : p.direct ? B * Hk : (int)segments;
     p.part_floats = p.balanced ? 2LL * p.workgroups * R * (D + 2) + 8LL * p.workgroups : 0;

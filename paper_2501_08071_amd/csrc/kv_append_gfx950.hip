@@ -12,8 +12,11 @@
 //   * the row's own loads do not depend on that and are under way meanwhile;
 //   * a thread's unit of work is two chunks of 8 elements, the two halves of 8 rotated pairs; with 2, 4 or 8 units a head it is the
 //     same unit in every head it visits, so a thread loads its angles once.
-// Measured (us; 32 query and 8 key heads of 128): 64 tokens 3.5 on the GPU, 9947 tokens of 6 sequences 51 (4.8 TB/s; four tokens a
-// workgroup 54, 512 threads instead of 256 52), 8000 tokens with 64 query heads 66 (73 and 64).
+// Measured (us; 32 query and 8 key heads of 128): 64 tokens 3.2 in a replayed graph, 9947 tokens of 6 sequences 50 (4.9 TB/s; four tokens a
+// workgroup 54, beside 51 with the kernel of then).  With 512 threads instead of 256, in turn: 3.0 and 3.2, 49.5 and 49.8; 8000 tokens with 64 query
+// heads on the same inputs again and again 62.0 and 62.9.
+// Every workgroup looks at all sequences: 1024 sequences of a token each 6.9 us (3.6 TB/s), 4096 28 (512 threads 26), 16384 226 (191; 1.8 TB/s): from
+// some thousands of sequences in a step on, the search is what it waits for.
 #include <hip/hip_runtime.h>
 #include <cstdint>
 

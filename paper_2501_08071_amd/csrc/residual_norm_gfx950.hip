@@ -12,7 +12,9 @@
 // Layout: TPR threads share a row, each holds CH chunks of 8 elements (16 bytes) in registers, chunk c of thread t at elements
 // 8 (c TPR + t): a wavefront's access is 1 KiB of consecutive bytes.  128 columns are 16 neighbouring lanes.  A row length that
 // is no multiple of 8 has a last chunk of 1 to 7 elements.
-// Measured, bfloat16: 16384 x 4096 to 8 bits 81 us (5.8 TB/s), to 16 bits 93 us (5.8); 16 x 4096 3.4 us on the GPU.
+// Measured, bfloat16: 16384 x 4096 to 8 bits 81 us (5.8 TB/s), to 16 bits 93 us (5.8); 16 x 4096 2.9 us in a replayed graph.  A batch of 333 rows of binary16, to
+// 8 bits with group scales, likewise: 4.3 us of 4096 elements, 5.1 of 5000 (512 threads instead of 256, 39 % of their places empty), 6.2 of 5001 (odd addresses).
+// Rows past 32768 elements are read twice in accesses of 2 bytes: 1100 x 32776, binary16, 105 us to 16 bits and 197 to 8, where 1100 x 32768 takes 55 and 49.
 // Rows of more than 16384 elements at odd addresses to 8 bits keep 13 or 14 words a thread in memory: 1024 threads have 128 registers each.
 #include <hip/hip_runtime.h>
 #include <cstdint>
